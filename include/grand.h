@@ -228,7 +228,8 @@ const char* grand_last_error(const grand_index* idx);
  *
  * What a call finds wrong in device data - a page id outside the pool, a position outside the rotary table, a
  * length beyond the table - it skips or clips, never following it, and records in a status word that
- * grand_cache_status reads back. */
+ * grand_cache_status reads back.  A token whose page is outside the pool takes no part: a search that pads
+ * its answer with GRAND_INVALID_ID may be attended at its full length. */
 typedef struct grand_cache grand_cache; /* opaque */
 
 typedef struct {

@@ -89,16 +89,20 @@ __global__ void __launch_bounds__(kWarps * 32, 8 / kWarps) attend_stream_kernel(
     lim_all = __reduce_min_sync(0xFFFFFFFFu, lim_all);
     low_all = __reduce_max_sync(0xFFFFFFFFu, low_all);
 
-    // tile t's 16 keys of this warp start at lo + t * kTile + warp * kKeys; lane r (and r + 16) looks up the place of key r
+    // tile t's 16 keys of this warp start at lo + t * kTile + warp * kKeys; lane r (and r + 16) looks up the place of key r:
+    // -1 behind the last key, kNoPage where the table names no page of the pool (such a token takes no part)
+    constexpr int64_t kNoPage = -2;
     auto place = [&](int t) -> int64_t {
       const int j = it.lo + t * kTile + warp * kKeys + (lane & 15);
       if (t >= t1 || j >= it.hi) return -1;
       const uint32_t jp = div_fast((uint32_t)j, a.pool.page);
       const int p = page_of(table, jp, a.pool.num_pages, a.status);
-      return p < 0 ? -1 : p * a.pool.page_stride + (j - (int)(jp * a.pool.page.d)) * a.pool.slot_stride + head_at;
+      return p < 0 ? kNoPage : p * a.pool.page_stride + (j - (int)(jp * a.pool.page.d)) * a.pool.slot_stride + head_at;
     };
+    bool gaps = false;   // such a token is among the tiles fetched so far; which it is is then looked up again at its tile
     auto fetch = [&](int stage, int64_t where) {
       const uint32_t kd = ring + stage * 2 * kRowsBytes, vd = kd + kRowsBytes;
+      gaps |= __any_sync(0xFFFFFFFFu, where == kNoPage);
       constexpr int C = L::kChunks, N = kKeys * C / 32;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -132,6 +136,7 @@ __global__ void __launch_bounds__(kWarps * 32, 8 / kWarps) attend_stream_kernel(
       const uint32_t ks0 = ring + stage * 2 * kRowsBytes, vs0 = ks0 + kRowsBytes;
       stage = stage + 1 == kStages ? 0 : stage + 1;
       const int j0 = it.lo + t * kTile + warp * kKeys;
+      const uint32_t gone = gaps ? __ballot_sync(0xFFFFFFFFu, place(t) == kNoPage) : 0u;   // bit r: key r is such a token
 
       float s[MT][2][4];
 #pragma unroll
@@ -154,7 +159,7 @@ __global__ void __launch_bounds__(kWarps * 32, 8 / kWarps) attend_stream_kernel(
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         float top[2] = {kNegInf, kNegInf};
-        if (j0 + kKeys - 1 <= lim_all && j0 >= low_all) {
+        if (j0 + kKeys - 1 <= lim_all && j0 >= low_all && gone == 0) {
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -164,9 +169,9 @@ __global__ void __launch_bounds__(kWarps * 32, 8 / kWarps) attend_stream_kernel(
           for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int j = j0 + n * 8 + (lane & 3) * 2 + (i & 1);
+              const int r = n * 8 + (lane & 3) * 2 + (i & 1), j = j0 + r;
               // a masked place takes no part, whatever its key holds
-              s[mt][n][i] = j <= lim[mt][i >> 1] && j >= low[mt][i >> 1] ? s[mt][n][i] * a.scale_log2 : kNegInf;
+              s[mt][n][i] = j <= lim[mt][i >> 1] && j >= low[mt][i >> 1] && !(gone >> r & 1) ? s[mt][n][i] * a.scale_log2 : kNegInf;
             }
         }
 #pragma unroll

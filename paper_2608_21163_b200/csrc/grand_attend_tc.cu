@@ -57,6 +57,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   __shared__ uint32_t tmem_at;
   __shared__ int gave_up;
   __shared__ uint32_t last_part[2];
+  __shared__ volatile int gaps;   // the table named a page outside the pool for a token of this block's tiles
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t smem = (uint32_t)__cvta_generic_to_shared(raw);
   float* shared_row = reinterpret_cast<float*>(raw + T::kShared);   // [row tile][half of the keys][row]: maxima, at the end sums
@@ -69,6 +70,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 
   if (tid == 0) {
     gave_up = 0;
+    gaps = 0;
     for (int i = 0; i < RING; ++i) bar_init(bars.full(i), 1), bar_init(bars.empty(i), 1);
     for (int t = 0; t < 2; ++t) bar_init(bars.q(t), 8), bar_init(bars.s(t), 1), bar_init(bars.p(t), 8), bar_init(bars.o(t), 1);
     bar_init(bars.drain(), 1);
@@ -95,13 +97,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     uint32_t phase = 1;  // the ring starts empty
     Boxes now, next;
     const int32_t* table = a.seq.table + (int64_t)it.b * a.seq.table_stride;
-    find_boxes(now, a.pool, table, maps, it.lo + t0 * kTile, it.hi, lane, a.status);
+    // (the flag is passed on by the barrier of the tile's load)
+    auto look_up = [&](Boxes& boxes, int j0) {
+      if (find_boxes(boxes, a.pool, table, maps, j0, it.hi, lane, a.status)) gaps = 1;
+    };
+    look_up(now, it.lo + t0 * kTile);
     bool ok = true;
     uint32_t issued = 0, parity = 0;  // stages that loads went to, and the parity of their last phase
     while (ok) {
       const int t1 = run.last(it, t0, at);
       for (int t = t0; t < t1 && ok; ++t) {
-        if (t + 1 < t1) find_boxes(next, a.pool, table, maps, it.lo + (t + 1) * kTile, it.hi, lane, a.status);
+        if (t + 1 < t1) look_up(next, it.lo + (t + 1) * kTile);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if (!(ok = bar_wait(bars.empty(stage), phase, &gave_up))) break;
@@ -119,7 +125,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       next_item<kRows, kTile>(a, it);
       t0 = 0;
       table = a.seq.table + (int64_t)it.b * a.seq.table_stride;
-      find_boxes(now, a.pool, table, maps, it.lo, it.hi, lane, a.status);
+      look_up(now, it.lo);
     }
     if (!ok)  // after a wait that ran out: leave nothing in flight towards this block's memory
       for (int i = 0; i < RING; ++i) {
@@ -163,11 +169,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       if (elect_one()) tc_commit(bars.empty(st));
       __syncwarp();
     };
+    // A token without a page takes no part.  Its key, loaded as zeros, becomes NaN, and so do its scores: the softmax of a tile
+    // without such tokens has nothing to ask, and one that meets a NaN looks for them.
+    auto mark_gaps = [&](int k_stage, int j) {
+      if (!gaps) return;
+      const int32_t* table = a.seq.table + (int64_t)it.b * a.seq.table_stride;
+      for (int r = lane; r < kTile; r += 32) {
+        const int key = it.lo + j * kTile + r;
+        if (key < it.hi && page_of(table, div_fast((uint32_t)key, a.pool.page), a.pool.num_pages, nullptr) < 0)
+          for (int x = 0; x < 8 * T::kCols; ++x)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring_at + k_stage * T::kQ + (x >> 3) * 16384 + r * 128 + (x & 7) * 16), "r"(-1) : "memory");
+      }
+      fence_async_smem();
+      __syncwarp();
+    };
     while (ok) {
       const int t1 = run.last(it, t0, at);
       const int tiles2 = it.m * (int)a.group.d - it.rt * kRows > 128 ? 2 : 1;   // row tiles with rows
       // S of the first keys
       if (!(ok = bar_wait(bars.full(stage), phase, &gave_up))) break;
+      mark_gaps(stage, t0);
       for (int t = 0; t < tiles2; ++t) {
         if (!(ok = bar_wait(bars.q(t), n_item[t] & 1, &gave_up))) break;
         tc_fence_after();
@@ -198,6 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         if (more) {
           if (!(ok = bar_wait(bars.full(k_stage), phase, &gave_up))) break;
           if (++stage == RING) stage = 0, phase ^= 1;
+          mark_gaps(k_stage, j + 1);
         }
         for (int t = 0; t < tiles2; ++t) {
           if (!(ok = bar_wait(bars.p(t), n_tile[t] & 1, &gave_up))) break;
@@ -278,16 +300,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           const bool plain = scale > 0.0f && last >= 63 && first <= 0 && fabsf(best) < __int_as_float(0x7F800000);
           const bool fast = __all_sync(0xFFFFFFFFu, plain);
           if (!fast) {
+            const bool look = __any_sync(0xFFFFFFFFu, best != best);   // for tokens without a page, one of 32 a lane
             best = kNegInf;   // (a negative scale turns the order around; a NaN does not raise the maximum)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
+            auto mask = [&](int c, uint32_t gone) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 // -inf in a masked place, whatever the key holds
-                const float x = c * 32 + i > last || c * 32 + i < first ? kNegInf : __uint_as_float(s[c][i]) * scale;
+                const float x = c * 32 + i > last || c * 32 + i < first || (gone >> i & 1) ? kNegInf : __uint_as_float(s[c][i]) * scale;
                 s[c][i] = __float_as_uint(x);
                 best = fmaxf(best, x);
               }
+            };
+            if (look) {
+              const int32_t* table = a.seq.table + (int64_t)it.b * a.seq.table_stride;
+              const int key = it.lo + j * kTile + side * 64 + lane;
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+                mask(c, __ballot_sync(0xFFFFFFFFu, key + c * 32 < it.hi && page_of(table, div_fast((uint32_t)(key + c * 32), a.pool.page), a.pool.num_pages, nullptr) < 0));
+            } else {
+              mask(0, 0);
+              mask(1, 0);
+            }
           }
           {  // the row's maximum over both sides
             float* mine = shared_row + t * 256 + r_in;   // (read by all before the next S, which waits for their P)

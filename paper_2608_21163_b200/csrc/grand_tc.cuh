@@ -172,15 +172,19 @@ __device__ __forceinline__ void pair_sync(int t) {  // the 256 threads of warpgr
 
 // Where the boxes of a tile of 128 keys lie: lane l looks up those that start at key j0 + (l + 32 i) * rows.  A box from
 // `hi` on, or of a page outside the pool, gets the page behind the last, which loads as zeros.  Where rows are gathered, lane
-// l looks up keys j0 + 4 l + i: `page` is the row's number in the list for head 0, or the one behind the last.
+// l looks up keys j0 + 4 l + i: `page` is the row's number in the list for head 0, or the one behind the last.  Returns (to
+// every lane of its own) whether a page that it looked up is outside the pool.
 struct Boxes {
   int page[4], slot[4];
 };
-__device__ __forceinline__ void find_boxes(Boxes& b, const PoolView& pool, const int32_t* table, const PoolMaps& maps, int j0, int hi, int lane, uint32_t* status) {
+__device__ __forceinline__ bool find_boxes(Boxes& b, const PoolView& pool, const int32_t* table, const PoolMaps& maps, int j0, int hi, int lane, uint32_t* status) {
+  bool gap = false;
   auto look_up = [&](int j, int& slot) {
     const uint32_t jp = div_fast((uint32_t)j, pool.page);
     slot = j - (int)(jp * pool.page.d);
-    return page_of(table, jp, pool.num_pages, status);
+    const int p = page_of(table, jp, pool.num_pages, status);
+    gap |= p < 0;
+    return p;
   };
   if (maps.gather) {
 #pragma unroll
@@ -193,7 +197,7 @@ __device__ __forceinline__ void find_boxes(Boxes& b, const PoolView& pool, const
         if (p >= 0) b.page[i] = (int)(p * maps.page_step + slot * maps.slot_step);
       }
     }
-    return;
+    return gap;
   }
   const int n = 128 / (int)maps.rows;
 #pragma unroll
@@ -206,6 +210,7 @@ __device__ __forceinline__ void find_boxes(Boxes& b, const PoolView& pool, const
       if (p >= 0) b.page[i] = p;
     }
   }
+  return gap;
 }
 // One tile of 128 keys, COLS blocks of 64 entries, into `dst` (COLS x 16 KB).
 template <int COLS>
