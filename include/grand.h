@@ -326,9 +326,11 @@ int grand_cache_weigh(grand_cache* cache, const grand_pool* pool, const grand_se
 /* Eviction: sequences of more than `keep` tokens keep the first `sinks`, the last `recent`, and of the others those
  * with the largest weights (ties: the lowest index; a NaN counts as the smallest), `keep` in all; the kept tokens'
  * keys, values and weights move together in their order.  With weight_groups > 1 every kv head chooses for itself.
+ * A token whose page is outside the pool is never kept; if it is a sink or among the last, another takes its place.  A kept
+ * token whose new slot is outside the pool is lost.
  * into: a table (batch x into_pages_per_seq, rows into_stride entries apart) of the pages that receive them, all
  * other than the source pages; NULL: in place.  kept_out: batch x weight_groups x keep, ascending, -1 behind the
- * last; lens_out: batch.  seqs->cu_new is not read.  keep >= sinks + recent, keep >= 1. */
+ * last; lens_out: batch, the number of tokens kept.  seqs->cu_new is not read.  keep >= sinks + recent, keep >= 1. */
 int grand_cache_evict(grand_cache* cache, const grand_pool* pool, const grand_seqs* seqs, uint32_t keep, uint32_t sinks,
                       uint32_t recent, const int32_t* into, int64_t into_stride, uint32_t into_pages_per_seq,
                       int32_t* kept_out, int32_t* lens_out, grand_stream stream);

@@ -270,7 +270,7 @@ class TokenCache:
     def evict(self, page_table, kv_lens, keep, sinks=0, recent=0, into=None):
         """Brings every sequence down to `keep` tokens: its first `sinks`, its last `recent` and the heaviest of the others (ties:
         the lowest index), moved together in their order, in place or into the pages of the table `into` (other pages than
-        the sequences').  Returns the kept tokens' indices [batch, groups, keep], -1 behind the last, and the new lengths."""
+        the sequences').  Tokens without a page are not kept.  Returns the kept tokens' indices [batch, groups, keep], -1 behind the last, and the new lengths."""
         hold = self._sequences(page_table, kv_lens, None, page_table.shape[0])
         batch = page_table.shape[0]
         if into is not None:

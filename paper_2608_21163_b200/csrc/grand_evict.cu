@@ -5,7 +5,8 @@
 // values.  Every block of a cluster has an equal run of the tokens and holds its keys in shared memory (where they fit; else
 // it reads them anew); three passes count the keys' digits (11, 11 and 10 bits) from the top, each block adds up the
 // cluster's counts, and narrow down to the smallest kept key T; then every key above T and the first ones equal to it are
-// taken, in order of the tokens, each block knowing from the others' counts where its run of the list begins.
+// taken, in order of the tokens, each block knowing from the others' counts where its run of the list begins.  A token whose
+// page is outside the pool is never kept; sinks and newest ones of that kind leave their places to the free tokens.
 // Move: 2 x 2 x kept x row bytes, bound by memory.
 #include <cooperative_groups.h>
 
@@ -20,9 +21,10 @@ constexpr int kSelect = 1024, kBins = 2048, kMaxCluster = 8;   // (two digits a 
 constexpr int kHeld = 24 * 1024;   // keys that a block holds
 constexpr int kCopies = 8;
 
-// Larger weight, larger key; -0 counts as 0 and a NaN as less than everything.
+// Larger weight, larger key; -0 counts as 0 and a NaN as less than everything.  Key 0 is left to tokens without a page.
+constexpr uint32_t kNoPage = 0;
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  if (!(w == w)) return 0u;
+  if (!(w == w)) return 1u;
   const uint32_t u = __float_as_uint(w + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -33,7 +35,8 @@ __global__ void __launch_bounds__(kSelect) select_kernel(const __grid_constant__
   // other: the lanes of a warp share kCopies counts of a digit.
   __shared__ uint32_t warp_sum[kSelect / 32], warp_equal[kSelect / 32];
   __shared__ uint32_t sh_digit, sh_left;
-  __shared__ uint32_t counts[2];     // of this block's free tokens: above T, equal to T
+  __shared__ uint32_t counts[2];     // of this block's tokens: kept whatever the equal ones are, free and equal to T
+  __shared__ uint32_t gaps;          // of its sinks and newest tokens: without a page
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
   uint32_t* hist = shared;
@@ -47,13 +50,20 @@ __global__ void __launch_bounds__(kSelect) select_kernel(const __grid_constant__
   const Seq s = load_seq(view, b, speaks ? a.status : nullptr);
   const int n = s.len, keep = (int)a.keep;
   int32_t* kept = a.kept + (int64_t)row * keep;
-  if (speaks) a.lens_out[b] = min(n, keep);
-  if (n <= keep) {  // (the whole cluster)
-    for (int i = rank * kSelect + tid; i < keep; i += blocks * kSelect) kept[i] = i < n ? i : -1;
-    return;
-  }
   const int32_t* table = a.seq.table + (int64_t)b * a.seq.table_stride;
-  const int lo = (int)a.sinks, hi = n - (int)a.recent;  // the free tokens (keep >= sinks + recent, so lo < hi)
+  const bool fits = n <= keep;
+  if (fits) {  // all stay if they have a page (every block looks at the whole table row: the cluster agrees)
+    bool gap = false;
+    for (int i = tid; i < (int)div_fast((uint32_t)(n + (int)a.pool.page.d - 1), a.pool.page); i += kSelect)
+      gap |= page_of(table, (uint32_t)i, a.pool.num_pages, a.status) < 0;
+    if (!__syncthreads_or(gap)) {
+      if (speaks) a.lens_out[b] = n;
+      for (int i = rank * kSelect + tid; i < keep; i += blocks * kSelect) kept[i] = i < n ? i : -1;
+      return;
+    }
+  }
+  // the free tokens (keep >= sinks + recent, so lo < hi); where all fit there are none
+  const int lo = fits ? n : (int)a.sinks, hi = fits ? n : n - (int)a.recent;
   // this block's run: a multiple of 32 tokens per warp
   const int per_warp = (n + blocks * kSelect - 1) / (blocks * kSelect) * 32, per_block = per_warp * (kSelect / 32);
   const int j0 = min(rank * per_block, n), j1 = min(j0 + per_block, n);
@@ -61,16 +71,17 @@ __global__ void __launch_bounds__(kSelect) select_kernel(const __grid_constant__
   auto read_key = [&](int j) -> uint32_t {
     const uint32_t jp = div_fast((uint32_t)j, a.pool.page);
     const int p = page_of(table, jp, a.pool.num_pages, a.status);
-    return p < 0 ? 0u : weight_key(__ldg(a.pool.weights + ((int64_t)p * groups + g) * a.pool.page.d + (j - (int)(jp * a.pool.page.d))));
+    return p < 0 ? kNoPage : weight_key(__ldg(a.pool.weights + ((int64_t)p * groups + g) * a.pool.page.d + (j - (int)(jp * a.pool.page.d))));
   };
   const bool holds = per_block <= kHeld;
   auto key = [&](int j) -> uint32_t { return holds ? held[j - j0] : read_key(j); };
   auto is_free = [&](int j) { return j < w1 && j >= lo && j < hi; };
-  uint32_t left = (uint32_t)(keep - (lo + n - hi)), prefix = 0;  // to take among the keys that start with `prefix`
-  const bool none = left == 0;
+  uint32_t left = 0, prefix = 0;     // to take among the keys that start with `prefix`
+  bool none = true, all = false;     // no free token is kept; all with a page are
   const int top = kBins - 2 - 2 * tid;   // the two digits of this thread, from the top
   uint32_t* mine = hist + (lane & (kCopies - 1)) * kBins;
   for (int i = tid; i < kCopies * kBins; i += kSelect) hist[i] = 0;
+  if (tid == 0) gaps = 0;
   __syncthreads();
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
@@ -79,14 +90,18 @@ __global__ void __launch_bounds__(kSelect) select_kernel(const __grid_constant__
       for (int j = w0 + lane; j < w1; j += 32) {
         const uint32_t k = read_key(j);
         if (holds) held[j - j0] = k;
-        if (is_free(j)) atomicAdd(&mine[k >> 21], 1u);
+        if (k == kNoPage) {
+          if (!is_free(j)) atomicAdd(&gaps, 1u);
+        } else if (is_free(j)) {
+          atomicAdd(&mine[k >> 21], 1u);
+        }
       }
     } else {
       const int shift = pass == 1 ? 10 : 0;
 #pragma unroll 4
       for (int j = w0 + lane; j < w1; j += 32) {
         const uint32_t k = key(j);
-        if (is_free(j) && (k >> (pass == 1 ? 21 : 10)) == prefix) atomicAdd(&mine[(k >> shift) & (pass == 1 ? 2047u : 1023u)], 1u);
+        if (is_free(j) && k != kNoPage && (k >> (pass == 1 ? 21 : 10)) == prefix) atomicAdd(&mine[(k >> shift) & (pass == 1 ? 2047u : 1023u)], 1u);
       }
     }
     __syncthreads();
@@ -110,6 +125,15 @@ __global__ void __launch_bounds__(kSelect) select_kernel(const __grid_constant__
           own.y += v.y;
         }
     }
+    if (pass == 0) {
+      uint32_t without = gaps;
+      if (blocks > 1) {
+        without = 0;
+        for (int r = 0; r < blocks; ++r) without += *cluster.map_shared_rank(&gaps, r);
+      }
+      left = (uint32_t)keep - ((uint32_t)(lo + n - hi) - without);
+      none = left == 0;
+    }
     // the digit at which the count from the top reaches `left`
     uint32_t incl = own.x + own.y;
 #pragma unroll
@@ -125,25 +149,32 @@ __global__ void __launch_bounds__(kSelect) select_kernel(const __grid_constant__
       const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, before, o);
       if (lane >= o) before += v;
     }
+    if (pass == 0) {   // fewer free tokens than places?
+      const uint32_t there = __shfl_sync(0xFFFFFFFFu, before, 31);
+      all = there <= left;
+      if (speaks) a.lens_out[b] = all ? keep - (int)(left - there) : keep;
+    }
     before = __shfl_sync(0xFFFFFFFFu, before, warp) - warp_sum[warp];   // of the warps before this one
     const uint32_t above = before + incl - (own.x + own.y);
     if (above < left && left <= above + own.y) sh_digit = (uint32_t)top + 1, sh_left = left - above;
     else if (above + own.y < left && left <= above + own.y + own.x) sh_digit = (uint32_t)top, sh_left = left - above - own.y;
     __syncthreads();
-    if (!none) {
+    if (!none && !all) {
       prefix = (prefix << (pass == 0 ? 0 : pass == 1 ? 11 : 10)) | sh_digit;
       left = sh_left;
     }
   }
-  // ---- how many keys above T and equal to it each warp's run has, and each block's
+  if (none || all) prefix = none ? 0xFFFFFFFFu : kNoPage, left = 0;   // (no key is that large)
+  // ---- how many tokens each warp's run has, and each block's, that are kept anyway (with a page, and not free or above T), and
+  // how many are equal to T
   uint32_t above = 0, equal = 0;
 #pragma unroll 4
-  for (int j = w0 + lane; j < w1; j += 32)
-    if (is_free(j) && !none) {
-      const uint32_t k = key(j);
-      above += k > prefix;
-      equal += k == prefix;
-    }
+  for (int j = w0 + lane; j < w1; j += 32) {
+    const uint32_t k = key(j);
+    if (k == kNoPage) continue;
+    above += !is_free(j) || k > prefix;
+    equal += is_free(j) && k == prefix;
+  }
   above = __reduce_add_sync(0xFFFFFFFFu, above);
   equal = __reduce_add_sync(0xFFFFFFFFu, equal);
   if (lane == 0) warp_sum[warp] = above, warp_equal[warp] = equal;
@@ -164,23 +195,27 @@ __global__ void __launch_bounds__(kSelect) select_kernel(const __grid_constant__
       above0 += other[0];
       equal0 += other[1];
     }
+  } else {
+    __syncthreads();
   }
-  if (none) left = 0;
-  // kept before token w0: the sinks and recent ones among them, the keys above T, and the first `left` equal ones
-  uint32_t at = above0 + min(equal0, left) + (uint32_t)min(w0, lo) + (uint32_t)max(0, w0 - hi);
+  uint32_t at = above0 + min(equal0, left);   // kept before token w0
 #pragma unroll 4
   for (int base = w0; base < w1; base += 32) {
     const int j = base + lane;
-    const bool in = j < w1, free_one = is_free(j);
-    const uint32_t k = free_one && !none ? key(j) : 0u;
-    const bool same = free_one && !none && k == prefix;
+    const uint32_t k = j < w1 ? key(j) : kNoPage;
+    const bool same = is_free(j) && k != kNoPage && k == prefix;
     const uint32_t me = __ballot_sync(0xFFFFFFFFu, same), below = (1u << lane) - 1;
-    const bool take = in && (!free_one || (!none && (k > prefix || (same && equal0 + __popc(me & below) < left))));
+    const bool take = k != kNoPage && (!is_free(j) || k > prefix || (same && equal0 + __popc(me & below) < left));
     equal0 += __popc(me);
     const uint32_t mt = __ballot_sync(0xFFFFFFFFu, take);
     const uint32_t to = at + __popc(mt & below);
     if (take && to < (uint32_t)keep) kept[to] = j;
     at += __popc(mt);
+  }
+  if (all) {   // behind the last: the tokens that are kept are the total of all blocks' runs
+    uint32_t total = 0;
+    for (int r = 0; r < blocks; ++r) total += blocks > 1 ? *cluster.map_shared_rank(counts, r) : counts[0];
+    for (int i = (int)total + rank * kSelect + tid; i < keep; i += blocks * kSelect) kept[i] = -1;
   }
   if (blocks > 1) cluster.sync();  // no block leaves while another reads its counts
 }
@@ -249,7 +284,7 @@ __global__ void __launch_bounds__(kSlide) slide_kernel(const __grid_constant__ E
   SeqView view = a.seq;
   view.cu = nullptr;
   const Seq s = load_seq(view, b, nullptr);
-  if (s.len <= (int)a.keep) return;  // nothing moves
+  if (a.lens_out[b] == s.len) return;  // nothing moves
   const int32_t* table = a.seq.table + (int64_t)b * a.seq.table_stride;
   const int32_t* kept = a.kept + ((int64_t)b * groups + g) * a.keep;
   const int64_t head_at = (int64_t)((groups == 1 ? 0 : g) + (int)(which >> 1)) * a.pool.head_stride + col * 16 + (threadIdx.x & 1) * 8;

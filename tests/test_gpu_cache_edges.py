@@ -93,3 +93,47 @@ def test_a_padded_list_of_rows_is_its_rows(qh, new):
 @pytest.mark.parametrize("dim,page,groups", [(64, 1, 1), (128, 16, 2), (96, 5, 2)])
 def test_weigh_with_tokens_without_a_page(lens, news, dim, page, groups):
     Holes(lens, news, 0.3, qh=8, kvh=2, dim=dim, page=page, groups=groups).check_weigh()
+
+
+def kept_with_gaps(w, valid, keep, sinks, recent):
+    n, valid = len(valid), valid.tolist()
+    if n <= keep:
+        return [j for j in range(n) if valid[j]]
+    rank = [(-math.inf if x != x else x) for x in w.tolist()]
+    fixed = [j for j in (*range(sinks), *range(n - recent, n)) if valid[j]]
+    free = sorted((j for j in range(sinks, n - recent) if valid[j]), key=lambda j: (-rank[j], j))
+    return sorted(fixed + free[: keep - len(fixed)])
+
+
+@pytest.mark.parametrize("inplace", [True, False])
+@pytest.mark.parametrize("lens,keep,sinks,recent,page,kvh,dim,groups,share", [
+    ([300, 40, 257, 0], 64, 4, 16, 16, 2, 64, 2, 0.3), ([300, 64, 257], 64, 40, 24, 1, 2, 40, 1, 0.3), ([300, 1], 64, 0, 0, 16, 1, 64, 1, 0.9),
+    ([300, 20], 32, 32, 0, 5, 2, 64, 2, 0.4), ([9000, 30, 8200], 3000, 16, 100, 7, 1, 8, 1, 0.3), ([20000], 19000, 0, 500, 16, 1, 8, 1, 0.3),
+    ([500, 300], 64, 4, 16, 16, 2, 64, 1, 1.0)])
+def test_evict_with_tokens_without_a_page(inplace, lens, keep, sinks, recent, page, kvh, dim, groups, share):
+    c = Holes(lens, [0] * len(lens), share, kvh=kvh, qh=kvh, dim=dim, page=page, groups=groups, spare=3 + len(lens) * -(-keep // page))
+    w = torch.rand(c.weights.shape, generator=c.g, device="cuda")
+    w = torch.where(w < 0.5, (w * 8).floor() / 8, w)
+    w[w > 0.99] = math.nan
+    c.weights.copy_(w)
+    into = None
+    if not inplace:
+        into = c.spare.nonzero().flatten()[: len(lens) * -(-keep // page)].view(len(lens), -1).to(torch.int32)
+    k0, v0, w0 = c.k.clone(), c.v.clone(), c.weights.clone()
+    want_k, want_v, want_w = k0.clone(), v0.clone(), w0.clone()
+    kept, new = c.cache.evict(c.table, c.kv_lens, keep, sinks=sinks, recent=recent, into=into)
+    for b, n in enumerate(lens):
+        p, s = c.where(b, n)
+        for g in range(groups):
+            ref = kept_with_gaps(w0[p, g, s], c.valid(b), keep, sinks, recent)
+            assert kept[b, g].tolist() == ref + [-1] * (keep - len(ref)) and int(new[b]) == len(ref)
+            j, i = torch.tensor(ref, device="cuda", dtype=torch.long), torch.arange(len(ref), device="cuda")
+            dp, ds = (c.table if inplace else into)[b].long()[i // page], i % page
+            there = (dp >= 0) & (dp < c.k.shape[0])      # a slot in a page outside the pool takes nothing
+            j, dp, ds = j[there], dp[there], ds[there]
+            want_w[dp, g, ds] = w0[p[j], g, s[j]]
+            for h in range(kvh) if groups == 1 else [g]:
+                want_k[dp, ds, h], want_v[dp, ds, h] = k0[p[j], s[j], h], v0[p[j], s[j], h]
+    for got, want in ((c.k, want_k), (c.v, want_v), (c.weights, want_w)):
+        assert torch.equal(got.nan_to_num(77.0), want.nan_to_num(77.0))
+    assert c.found() == 1
