@@ -293,7 +293,8 @@ int grand_rope(const void* x, void* out, uint32_t dtype, uint64_t tokens, uint32
                uint32_t interleaved, uint32_t inverse, grand_stream stream);
 
 /* New tokens enter the cache: q (may be NULL) is turned into q_out, k is turned and written with v into the slots
- * of the new tokens, kv_lens[b] - new .. kv_lens[b] - 1, whose weights become 0.  k, v: tokens x kv_heads x
+ * of the new tokens, kv_lens[b] - new .. kv_lens[b] - 1, whose weights become 0.  A token whose slot is not in the
+ * table, or whose sequence's bounds in cu_new are not rows of the call, is dropped.  k, v: tokens x kv_heads x
  * head_dim; q, q_out: tokens x q_heads x head_dim.  strides: six numbers, the token and head strides of q, k, v
  * (q_out is dense).  rot 0: no rotation (table and positions unused). */
 int grand_cache_append(grand_cache* cache, const grand_pool* pool, const grand_seqs* seqs, const void* q, void* q_out,

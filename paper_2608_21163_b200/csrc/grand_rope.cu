@@ -214,9 +214,13 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
   const float* row = table_row(a.q, t);
   const uint32_t b = a.seq.cu ? find_seq(a.seq.cu, a.seq.batch, (int)t) : (uint32_t)t;
   if (h0 < lanes) unit.angles(u0, a.q.rot, row, a.q.sign);
-  const Seq s = load_seq(a.seq, b, a.q.status);
-  const int slot = s.len - s.m + ((int)t - s.row);
-  const bool mine = (int)t >= s.row && (int)t < s.row + s.m && slot >= 0;  // a token before the cache's first slot is dropped
+  // The slot comes from the length and the bounds as they are: clipped ones would name the slot of another token.  A token whose
+  // slot the table does not reach (or before the first), or whose sequence's bounds are not rows of this call, is dropped.
+  const int len = a.seq.lens[b], lo = a.seq.cu ? a.seq.cu[b] : (int)b, hi = a.seq.cu ? a.seq.cu[b + 1] : lo + 1;
+  const bool bounds = 0 <= lo && lo <= hi && hi <= (int)a.seq.tokens;
+  const int slot = len - hi + (int)t;   // (used where 0 <= len and lo <= t < hi: no overflow)
+  const bool mine = bounds && (int)t >= lo && (int)t < hi && len >= 0 && (uint32_t)slot < a.seq.max_len;
+  if (!bounds || (uint32_t)len > a.seq.max_len) atomicOr(a.q.status, (uint32_t)kBadLength);
   int page = -1;
   uint32_t in_page = 0;
   if (mine) {

@@ -137,3 +137,31 @@ def test_evict_with_tokens_without_a_page(inplace, lens, keep, sinks, recent, pa
     for got, want in ((c.k, want_k), (c.v, want_v), (c.weights, want_w)):
         assert torch.equal(got.nan_to_num(77.0), want.nan_to_num(77.0))
     assert c.found() == 1
+
+
+# ---- lengths and bounds that do not fit
+
+@pytest.mark.parametrize("lens,cu,written", [
+    # written: slots of either sequence and the rows that they get
+    ([65, 40], None, ({}, {39: 1})),                                               # one slot past the table
+    ([66, 40], [0, 5, 8], ({61: 0, 62: 1, 63: 2}, {37: 5, 38: 6, 39: 7})),         # the last two of five past it
+    ([1 << 30, 40], [0, 5, 8], ({}, {37: 5, 38: 6, 39: 7})),
+    ([-3, 40], [0, 5, 8], ({}, {37: 5, 38: 6, 39: 7})),
+    ([64, 40], [0, 5, 12], ({59 + i: i for i in range(5)}, {})),                   # bounds past the rows of the call
+    ([64, 40], [-2, 5, 8], ({}, {37: 5, 38: 6, 39: 7})),
+    ([64, 40], [0, 6, 2], ({58 + i: i for i in range(6)}, {})),                    # bounds that descend
+])
+def test_append_writes_no_other_tokens_slot(lens, cu, written):
+    c = Case([64, 48], [1, 1] if cu is None else [5, 3], qh=4, kvh=2, dim=64, page=16)
+    c.weights.fill_(3.0)
+    k, v = (torch.randn((c.total, 2, 64), generator=c.g, device="cuda").to(BF16) for _ in range(2))
+    want_k, want_v, want_w = c.k.clone(), c.v.clone(), c.weights.clone()
+    for b in range(2):
+        for slot, row in written[b].items():
+            p, s = int(c.table[b, slot // 16]), slot % 16
+            want_k[p, s], want_v[p, s], want_w[p, :, s] = k[row], v[row], 0.0
+    c.cache.append(None, k, v, None, None, c.table, torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                   cu_new=None if cu is None else torch.tensor(cu, dtype=torch.int32, device="cuda"))
+    for got, want in ((c.k, want_k), (c.v, want_v), (c.weights, want_w)):
+        assert torch.equal(got.nan_to_num(77.0), want.nan_to_num(77.0))
+    assert c.cache.status() == 4
