@@ -331,7 +331,7 @@ int grand_cache_weigh(grand_cache* cache, const grand_pool* pool, const grand_se
  * token whose new slot is outside the pool is lost.
  * into: a table (batch x into_pages_per_seq, rows into_stride entries apart) of the pages that receive them, all
  * other than the source pages; NULL: in place.  kept_out: batch x weight_groups x keep, ascending, -1 behind the
- * last; lens_out: batch, the number of tokens kept.  seqs->cu_new is not read.  keep >= sinks + recent, keep >= 1. */
+ * last; lens_out: batch, the number of tokens kept; not kv_lens itself.  seqs->cu_new is not read.  keep >= sinks + recent, keep >= 1. */
 int grand_cache_evict(grand_cache* cache, const grand_pool* pool, const grand_seqs* seqs, uint32_t keep, uint32_t sinks,
                       uint32_t recent, const int32_t* into, int64_t into_stride, uint32_t into_pages_per_seq,
                       int32_t* kept_out, int32_t* lens_out, grand_stream stream);

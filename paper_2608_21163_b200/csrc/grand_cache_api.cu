@@ -256,6 +256,8 @@ int grand_cache_evict(grand_cache* c, const grand_pool* p, const grand_seqs* s, 
   if (into && (uint64_t)into_pages * c->o.page_size < keep) return fail(c, GRAND_ERR_INVALID_ARG, "the pages of `into` hold less than `keep` tokens");
   if (s->batch == 0) return GRAND_OK;
   if (!kept || !lens_out) return fail(c, GRAND_ERR_INVALID_ARG, "kept_out or lens_out is null");
+  // (lengths are read while others are written)
+  if (lens_out < s->kv_lens + s->batch && s->kv_lens < lens_out + s->batch) return fail(c, GRAND_ERR_INVALID_ARG, "lens_out must not be kv_lens");
   a.keep = keep; a.sinks = sinks; a.recent = recent;
   a.into = into; a.into_stride = into_stride;
   a.kept = kept; a.lens_out = lens_out;

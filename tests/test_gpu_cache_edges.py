@@ -165,3 +165,22 @@ def test_append_writes_no_other_tokens_slot(lens, cu, written):
     for got, want in ((c.k, want_k), (c.v, want_v), (c.weights, want_w)):
         assert torch.equal(got.nan_to_num(77.0), want.nan_to_num(77.0))
     assert c.cache.status() == 4
+
+
+def test_evict_refuses_to_write_the_lengths_that_it_reads():
+    import ctypes as C
+    c = Case([100, 50], [1, 1], qh=4, kvh=2, dim=64)
+    hold = c.cache._sequences(c.table, c.kv_lens, None, 2)
+    kept, after = torch.zeros((2, 2, 20), dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    both = torch.tensor([100, 50, 0, 0], dtype=torch.int32, device="cuda")
+
+    def evict(lens, out):
+        c.cache._seqs.kv_lens = lens.data_ptr()
+        stream = torch.cuda.current_stream().cuda_stream
+        return c.cache.lib.grand_cache_evict(c.cache.h, c.cache._pool_at, c.cache._seqs_at, 20, 0, 0, None, 0, 0, kept.data_ptr(), out.data_ptr(), C.c_void_p(stream))
+
+    assert evict(both, both) == -1 and b"lens_out" in c.cache.lib.grand_cache_last_error(c.cache.h)
+    assert evict(both, both[1:]) == -1 and evict(both[1:], both) == -1
+    assert evict(both, both[2:]) == 0 and both.tolist() == [100, 50, 20, 20]
+    assert evict(both, after[1:]) == 0 and after.tolist() == [0, 20, 20, 0]
+    del hold
