@@ -57,10 +57,16 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _int32(t, length, name):
-    if t.dtype != torch.int32 or not t.is_cuda or t.shape != (length,):
-        raise ValueError(f"{name} must be a CUDA int32 tensor of {length} entries")
+def _int32(t, length, name, device):
+    if t.dtype != torch.int32 or t.get_device() != device or t.shape != (length,):
+        raise ValueError(f"{name} must be an int32 tensor of {length} entries on CUDA device {device}")
     return t if t.is_contiguous() else t.contiguous()
+
+
+def _table(t, name, device):
+    if t.dtype != torch.int32 or t.get_device() != device or t.dim() != 2:
+        raise ValueError(f"{name} must be an int32 matrix on CUDA device {device}")
+    return t if t.stride(1) == 1 else t.contiguous()
 
 
 def _stream(device):
@@ -98,10 +104,10 @@ def rope_table(length, frequencies, magnitude=1.0, device="cuda"):
     return torch.cat([angle.cos(), angle.sin()], 1).mul_(magnitude).float()
 
 
-def _check_table(table, positions, tokens):
-    if table.dtype != torch.float32 or not table.is_cuda or table.dim() != 2 or not table.is_contiguous():
-        raise ValueError("table must be a dense float32 CUDA matrix")
-    return _int32(positions, tokens, "positions")
+def _check_table(table, positions, tokens, device):
+    if table.dtype != torch.float32 or table.get_device() != device or table.dim() != 2 or not table.is_contiguous():
+        raise ValueError(f"table must be a dense float32 matrix on CUDA device {device}")
+    return _int32(positions, tokens, "positions", device)
 
 
 def rope(x, table, positions, interleaved=False, inverse=False, out=None):
@@ -109,7 +115,7 @@ def rope(x, table, positions, interleaved=False, inverse=False, out=None):
     table.shape[1] entries of every head are turned by their token's angles, the others copied.  Pairs are (i, i + rot / 2),
     or (2i, 2i + 1) if interleaved.  inverse turns back, which is the gradient of the rotation.  out may be x."""
     _need(x.is_cuda and x.dim() == 3 and x.dtype in _DTYPE, "x must be a CUDA tensor [tokens, heads, dim] of a supported type")
-    positions = _check_table(table, positions, x.shape[0])
+    positions = _check_table(table, positions, x.shape[0], x.get_device())
     if x.stride(2) != 1:
         x = x.contiguous()
     if out is None:
@@ -150,7 +156,7 @@ class TokenCache:
         self.lib = _lib()
         self.k_pages, self.v_pages, self.weights = k_pages, v_pages, weights
         self.q_heads, self.kv_heads, self.head_dim, self.page_size, self.groups = q_heads or kv_heads, kv_heads, dim, size, groups
-        self.dtype, self.device = k_pages.dtype, k_pages.device
+        self.dtype, self.device, self.index = k_pages.dtype, k_pages.device, k_pages.get_device()
         o = _Options(q_heads=self.q_heads, kv_heads=kv_heads, head_dim=dim, dtype=_DTYPE.get(k_pages.dtype, 0), page_size=size,
                      weight_groups=groups, max_batch=max_batch, max_tokens=max_tokens, num_pages=pages)
         h = C.c_void_p()
@@ -182,13 +188,11 @@ class TokenCache:
 
     def _sequences(self, page_table, kv_lens, cu_new, tokens):
         """Fills the call's description; returns what has to live until the call is made."""
-        _need(page_table.dtype == torch.int32 and page_table.is_cuda and page_table.dim() == 2, "page_table must be a CUDA int32 matrix")
+        page_table = _table(page_table, "page_table", self.index)
         batch, per = page_table.shape
-        if page_table.stride(1) != 1:
-            page_table = page_table.contiguous()
-        kv_lens = _int32(kv_lens, batch, "kv_lens")
+        kv_lens = _int32(kv_lens, batch, "kv_lens", self.index)
         if cu_new is not None:
-            cu_new = _int32(cu_new, batch + 1, "cu_new")
+            cu_new = _int32(cu_new, batch + 1, "cu_new", self.index)
         s = self._seqs
         s.page_table, s.kv_lens, s.cu_new = page_table.data_ptr(), kv_lens.data_ptr(), None if cu_new is None else cu_new.data_ptr()
         s.table_stride, s.pages_per_seq, s.batch, s.tokens = page_table.stride(0), per, batch, tokens
@@ -214,9 +218,9 @@ class TokenCache:
             if q_out is None:
                 q_out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
             else:
-                _need(q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous(), "q_out must be dense and like q")
+                _need(q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.device == q.device and q_out.is_contiguous(), "q_out must be dense and like q")
         if table is not None:
-            positions = _check_table(table, positions, tokens)
+            positions = _check_table(table, positions, tokens, self.index)
         hold = self._sequences(page_table, kv_lens, cu_new, tokens)
         strides = self._strides
         if q is not None:
@@ -274,8 +278,8 @@ class TokenCache:
         hold = self._sequences(page_table, kv_lens, None, page_table.shape[0])
         batch = page_table.shape[0]
         if into is not None:
-            _need(into.dtype == torch.int32 and into.is_cuda and into.dim() == 2 and into.shape[0] == batch, "into must be a CUDA int32 matrix with a row per sequence")
-            into = into if into.stride(1) == 1 else into.contiguous()
+            into = _table(into, "into", self.index)
+            _need(into.shape[0] == batch, "into must have a row per sequence")
         kept = page_table.new_empty((batch, max(1, self.groups), keep))
         lens = page_table.new_empty(batch)
         self._check(self.lib.grand_cache_evict(

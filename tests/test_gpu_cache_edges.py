@@ -184,3 +184,29 @@ def test_evict_refuses_to_write_the_lengths_that_it_reads():
     assert evict(both, both[2:]) == 0 and both.tolist() == [100, 50, 20, 20]
     assert evict(both, after[1:]) == 0 and after.tolist() == [0, 20, 20, 0]
     del hold
+
+
+# ---- arguments that do not fit
+
+def test_tensors_elsewhere_are_refused():
+    """Every tensor has to be on the pool's device: a pointer to host memory must never reach a kernel."""
+    from paper_2608_21163_b200.cache import rope, rope_frequencies, rope_table
+    c = Case([100, 50], [1, 1], qh=4, kvh=2, dim=64)
+    k, table, at = c.q[:, :2].contiguous(), rope_table(128, rope_frequencies(64)), torch.tensor([99, 49], dtype=torch.int32, device="cuda")
+    spare = c.spare.nonzero().flatten()[:2].view(2, 1).to(torch.int32)
+    _, lse = c.cache.attend(c.q, c.table, c.kv_lens, cu_new=c.cu)
+    calls = {
+        "append": (c.cache.append, dict(q=c.q, k=k, v=k, table=table, positions=at, page_table=c.table, kv_lens=c.kv_lens, cu_new=c.cu, q_out=torch.empty_like(c.q))),
+        "attend": (c.cache.attend, dict(q=c.q, page_table=c.table, kv_lens=c.kv_lens, cu_new=c.cu, out=torch.empty_like(c.q), lse=torch.empty_like(lse))),
+        "weigh": (c.cache.weigh, dict(q=c.q, lse=lse, page_table=c.table, kv_lens=c.kv_lens, cu_new=c.cu)),
+        "evict": (c.cache.evict, dict(page_table=c.table, kv_lens=c.kv_lens, keep=16, into=spare)),
+        "rope": (rope, dict(x=c.q, table=table, positions=at, out=torch.empty_like(c.q)))}
+    for name, (call, kw) in calls.items():
+        for arg, t in kw.items():
+            if isinstance(t, torch.Tensor):
+                with pytest.raises(ValueError):
+                    call(**{**kw, arg: t.cpu()})
+        call(**kw)
+    with pytest.raises(ValueError):
+        rope_table_on_host = table.cpu()
+        rope(c.q.cpu(), rope_table_on_host, at.cpu())
