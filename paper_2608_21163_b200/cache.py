@@ -57,6 +57,13 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _count(x, name):
+    # ctypes would cut a number down to its low 32 bits
+    if not 0 <= x < 1 << 32:
+        raise ValueError(f"{name} must be a number from 0 below 2^32")
+    return x
+
+
 def _int32(t, length, name, device):
     if t.dtype != torch.int32 or t.get_device() != device or t.shape != (length,):
         raise ValueError(f"{name} must be an int32 tensor of {length} entries on CUDA device {device}")
@@ -157,6 +164,8 @@ class TokenCache:
         self.k_pages, self.v_pages, self.weights = k_pages, v_pages, weights
         self.q_heads, self.kv_heads, self.head_dim, self.page_size, self.groups = q_heads or kv_heads, kv_heads, dim, size, groups
         self.dtype, self.device, self.index = k_pages.dtype, k_pages.device, k_pages.get_device()
+        _need(0 < self.q_heads < 1 << 32, "q_heads must be a positive number")
+        max_batch, max_tokens = _count(max_batch, "max_batch"), _count(max_tokens, "max_tokens")
         o = _Options(q_heads=self.q_heads, kv_heads=kv_heads, head_dim=dim, dtype=_DTYPE.get(k_pages.dtype, 0), page_size=size,
                      weight_groups=groups, max_batch=max_batch, max_tokens=max_tokens, num_pages=pages)
         h = C.c_void_p()
@@ -254,7 +263,7 @@ class TokenCache:
         hold = self._sequences(page_table, kv_lens, cu_new, shape[0])
         self._check(self.lib.grand_cache_attend(
             self.h, self._pool_at, self._seqs_at, q.data_ptr(), q.stride(0), q.stride(1), self.head_dim ** -0.5 if scale is None else scale,
-            causal, window, out.data_ptr(), lse.data_ptr(), _stream(self.device)))
+            causal, _count(window, "window"), out.data_ptr(), lse.data_ptr(), _stream(self.device)))
         del hold
         return out, lse
 
@@ -267,7 +276,7 @@ class TokenCache:
         hold = self._sequences(page_table, kv_lens, cu_new, q.shape[0])
         self._check(self.lib.grand_cache_weigh(
             self.h, self._pool_at, self._seqs_at, q.data_ptr(), q.stride(0), q.stride(1), lse.data_ptr(),
-            self.head_dim ** -0.5 if scale is None else scale, causal, window, decay, _stream(self.device)))
+            self.head_dim ** -0.5 if scale is None else scale, causal, _count(window, "window"), decay, _stream(self.device)))
         del hold
         return self.weights
 
@@ -275,6 +284,7 @@ class TokenCache:
         """Brings every sequence down to `keep` tokens: its first `sinks`, its last `recent` and the heaviest of the others (ties:
         the lowest index), moved together in their order, in place or into the pages of the table `into` (other pages than
         the sequences').  Tokens without a page are not kept.  Returns the kept tokens' indices [batch, groups, keep], -1 behind the last, and the new lengths."""
+        keep, sinks, recent = _count(keep, "keep"), _count(sinks, "sinks"), _count(recent, "recent")
         hold = self._sequences(page_table, kv_lens, None, page_table.shape[0])
         batch = page_table.shape[0]
         if into is not None:

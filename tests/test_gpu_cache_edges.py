@@ -210,3 +210,19 @@ def test_tensors_elsewhere_are_refused():
     with pytest.raises(ValueError):
         rope_table_on_host = table.cpu()
         rope(c.q.cpu(), rope_table_on_host, at.cpu())
+
+
+@pytest.mark.parametrize("number", [-1, 1 << 32, (1 << 32) + 5])
+def test_numbers_that_32_bits_do_not_hold_are_refused(number):
+    from paper_2608_21163_b200.cache import TokenCache
+    c = Case([100, 50], [1, 1], qh=4, kvh=2, dim=64)
+    for call in (lambda: c.cache.attend(c.q, c.table, c.kv_lens, window=number),
+                 lambda: c.cache.weigh(c.q, torch.zeros(2, 4, device="cuda"), c.table, c.kv_lens, window=number),
+                 lambda: c.cache.evict(c.table, c.kv_lens, number), lambda: c.cache.evict(c.table, c.kv_lens, 16, sinks=number),
+                 lambda: c.cache.evict(c.table, c.kv_lens, 16, recent=number), lambda: TokenCache(c.k, c.v, q_heads=number),
+                 lambda: TokenCache(c.k, c.v, max_batch=number), lambda: TokenCache(c.k, c.v, max_tokens=number)):
+        with pytest.raises(ValueError):
+            call()
+    # the largest window that fits is as good as none
+    want, _ = c.cache.attend(c.q, c.table, c.kv_lens)
+    assert torch.equal(c.cache.attend(c.q, c.table, c.kv_lens, window=(1 << 32) - 1)[0], want)
