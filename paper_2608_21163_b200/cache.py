@@ -71,8 +71,10 @@ def _int32(t, length, name, device):
 
 
 def _table(t, name, device):
+    if t.dtype == torch.uint32:   # ids as a search returns them; its padding becomes -1, which is no page either
+        t = t.view(torch.int32)
     if t.dtype != torch.int32 or t.get_device() != device or t.dim() != 2:
-        raise ValueError(f"{name} must be an int32 matrix on CUDA device {device}")
+        raise ValueError(f"{name} must be an int32 or uint32 matrix on CUDA device {device}")
     return t if t.stride(1) == 1 else t.contiguous()
 
 
@@ -145,8 +147,9 @@ class TokenCache:
     [pages, kv heads, page size, head dim] is passed as its transpose(1, 2)).  weights: [pages, groups, page size] float32
     with groups 1 or kv heads, or None.  The methods run on the current stream; one object serves one stream at a time.
 
-    Every method takes page_table [batch, pages per sequence] and kv_lens [batch] (int32, on the GPU): the tokens cached for
-    each sequence, the new ones last among them.  The new tokens' rows are packed over the batch; cu_new [batch + 1] (int32)
+    Every method takes page_table [batch, pages per sequence] (int32, or the uint32 ids of a search) and kv_lens [batch] (int32), on
+    the GPU: the tokens cached for each sequence, the new ones last among them.  At most max_batch sequences a call (4,096 is
+    the limit) and max_tokens new tokens.  The new tokens' rows are packed over the batch; cu_new [batch + 1] (int32)
     says where each sequence's start, None means one new token per sequence.
     """
 
@@ -290,8 +293,8 @@ class TokenCache:
         if into is not None:
             into = _table(into, "into", self.index)
             _need(into.shape[0] == batch, "into must have a row per sequence")
-        kept = page_table.new_empty((batch, max(1, self.groups), keep))
-        lens = page_table.new_empty(batch)
+        kept = page_table.new_empty((batch, max(1, self.groups), keep), dtype=torch.int32)
+        lens = page_table.new_empty(batch, dtype=torch.int32)
         self._check(self.lib.grand_cache_evict(
             self.h, self._pool_at, self._seqs_at, keep, sinks, recent, None if into is None else into.data_ptr(),
             0 if into is None else into.stride(0), 0 if into is None else into.shape[1], kept.data_ptr(), lens.data_ptr(),

@@ -226,3 +226,18 @@ def test_numbers_that_32_bits_do_not_hold_are_refused(number):
     # the largest window that fits is as good as none
     want, _ = c.cache.attend(c.q, c.table, c.kv_lens)
     assert torch.equal(c.cache.attend(c.q, c.table, c.kv_lens, window=(1 << 32) - 1)[0], want)
+
+
+def test_the_ids_of_a_search_are_a_page_table():
+    """uint32, as they come, padding included, and non-contiguous too."""
+    c = Case([30] * 3, [1] * 3, qh=2, kvh=1, dim=64, page=1)
+    want, lse = c.cache.attend(c.q, c.table, c.kv_lens)
+    ids = c.table.view(torch.uint32)
+    padded = torch.full((3, 40), 0xFFFFFFFF, dtype=torch.int64, device="cuda").to(torch.uint32)
+    padded.view(torch.int32)[:, :30] = c.table
+    spread = padded.view(torch.int32).repeat_interleave(2, 1).view(torch.uint32)[:, ::2]
+    for table, n in ((ids, 30), (padded, 40), (spread, 40)):
+        got, got_lse = c.cache.attend(c.q, table, torch.full_like(c.kv_lens, n))
+        assert torch.equal(got, want) and torch.equal(got_lse, lse)
+    c.weights.zero_()
+    assert torch.equal(c.cache.evict(ids, c.kv_lens, 10, into=c.table[:, :10].clone().view(torch.uint32))[0].cpu(), torch.arange(10, dtype=torch.int32).expand(3, 1, 10))
