@@ -119,10 +119,46 @@ def _check_table(table, positions, tokens, device):
     return _int32(positions, tokens, "positions", device)
 
 
+class _Rope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, table, positions, interleaved, inverse):
+        ctx.save_for_backward(table, positions)
+        ctx.interleaved, ctx.inverse = interleaved, inverse
+        return rope(x, table, positions, interleaved, inverse)
+
+    @staticmethod
+    def backward(ctx, grad):
+        return rope(grad, *ctx.saved_tensors, ctx.interleaved, not ctx.inverse), None, None, None, None
+
+
+class _NoGradient(torch.autograd.Function):
+    # Marks the results of a call that has no gradient: a backward pass through them raises instead of losing what was asked.
+    @staticmethod
+    def forward(ctx, name, results, *tensors):   # the results, then the inputs
+        ctx.name = name
+        ctx.mark_dirty(*tensors[:results])
+        return tensors[:results]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(f"TokenCache.{ctx.name} has no gradient")
+
+
+def _wants_gradient(*tensors):
+    for t in tensors:
+        if t.requires_grad:
+            return torch.is_grad_enabled()
+    return False
+
+
 def rope(x, table, positions, interleaved=False, inverse=False, out=None):
     """Rotary positions of x [tokens, heads, dim] (float16, bfloat16 or float32, any token and head strides): the first
     table.shape[1] entries of every head are turned by their token's angles, the others copied.  Pairs are (i, i + rot / 2),
-    or (2i, 2i + 1) if interleaved.  inverse turns back, which is the gradient of the rotation.  out may be x."""
+    or (2i, 2i + 1) if interleaved.  inverse turns back, which is the gradient of the rotation; it is also what a backward pass
+    does where x requires a gradient (out is refused then, and the table is a constant).  out may be x."""
+    if _wants_gradient(x, table):
+        _need(out is None and not table.requires_grad, "rope gives a gradient to x alone, and not where out is given")
+        return _Rope.apply(x, table, positions, interleaved, inverse)
     _need(x.is_cuda and x.dim() == 3 and x.dtype in _DTYPE, "x must be a CUDA tensor [tokens, heads, dim] of a supported type")
     positions = _check_table(table, positions, x.shape[0], x.get_device())
     if x.stride(2) != 1:
@@ -150,7 +186,10 @@ class TokenCache:
     Every method takes page_table [batch, pages per sequence] (int32, or the uint32 ids of a search) and kv_lens [batch] (int32), on
     the GPU: the tokens cached for each sequence, the new ones last among them.  At most max_batch sequences a call (4,096 is
     the limit) and max_tokens new tokens.  The new tokens' rows are packed over the batch; cu_new [batch + 1] (int32)
-    says where each sequence's start, None means one new token per sequence.
+    says where each sequence's start, None means one new token per sequence.  Rows of no sequence are left as they are.
+
+    The methods have no gradient (`rope` has): a backward pass through what append or attend returned raises, and out, lse and q_out are
+    refused where one of the inputs requires a gradient.  What lies in the pool and its weights is never part of one.
     """
 
     def __init__(self, k_pages, v_pages, weights=None, q_heads=None, max_batch=256, max_tokens=8192):
@@ -227,10 +266,12 @@ class TokenCache:
         if q is not None:
             q = self._heads(q, self.q_heads, "q", tokens)
             q = q if q.stride(2) == 1 else q.contiguous()
+            wants = _wants_gradient(q, k, v)
             if q_out is None:
                 q_out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
             else:
                 _need(q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.device == q.device and q_out.is_contiguous(), "q_out must be dense and like q")
+                _need(not wants, "append has no gradient")
         if table is not None:
             positions = _check_table(table, positions, tokens, self.index)
         hold = self._sequences(page_table, kv_lens, cu_new, tokens)
@@ -245,6 +286,8 @@ class TokenCache:
             0 if table is None else table.shape[1], None if table is None else positions.data_ptr(), interleaved,
             _stream(self.device)))
         del hold
+        if q is not None and wants:
+            (q_out,) = _NoGradient.apply("append", 1, q_out, q, k, v)
         return None if q is None else q_out
 
     def attend(self, q, page_table, kv_lens, cu_new=None, scale=None, causal=True, window=0, out=None, lse=None):
@@ -252,6 +295,8 @@ class TokenCache:
         n tokens cached, sees token j if j <= n - m + i (causal) and, with a window, j > n - m + i - window.  scale defaults to
         1 / sqrt(dim).  Returns the output, like q, and the log of every row's sum [tokens, q heads]; a row that sees nothing
         gives 0 and -inf."""
+        wants = _wants_gradient(q)
+        _need(not wants or (out is None and lse is None), "attend has no gradient")
         q = _rows16(self._heads(q, self.q_heads, "q"))
         shape = q.shape
         if out is None:
@@ -268,7 +313,7 @@ class TokenCache:
             self.h, self._pool_at, self._seqs_at, q.data_ptr(), q.stride(0), q.stride(1), self.head_dim ** -0.5 if scale is None else scale,
             causal, _count(window, "window"), out.data_ptr(), lse.data_ptr(), _stream(self.device)))
         del hold
-        return out, lse
+        return _NoGradient.apply("attend", 2, out, lse, q) if wants else (out, lse)
 
     def weigh(self, q, lse, page_table, kv_lens, cu_new=None, scale=None, causal=True, window=0, decay=1.0):
         """Adds to every cached token's weight (times decay) the attention that the queries q pay it; lse is what `attend`

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from .test_gpu_cache import BF16, F16, UNIT, Case
+from .test_gpu_cache import BF16, F16, UNIT, Case, rope_ref_differentiable
 
 pytestmark = pytest.mark.gpu
 
@@ -241,3 +241,64 @@ def test_the_ids_of_a_search_are_a_page_table():
         assert torch.equal(got, want) and torch.equal(got_lse, lse)
     c.weights.zero_()
     assert torch.equal(c.cache.evict(ids, c.kv_lens, 10, into=c.table[:, :10].clone().view(torch.uint32))[0].cpu(), torch.arange(10, dtype=torch.int32).expand(3, 1, 10))
+
+
+# ---- gradients
+
+@pytest.mark.parametrize("dtype", [BF16, F16, torch.float32])
+@pytest.mark.parametrize("inter,inverse,dim,rot", [(False, False, 48, 32), (True, False, 64, 64), (False, True, 64, 64), (True, True, 40, 6)])
+def test_rope_takes_part_in_a_backward_pass(dtype, inter, inverse, dim, rot):
+    from paper_2608_21163_b200.cache import rope, rope_frequencies, rope_table
+    g = torch.Generator(device="cuda"); g.manual_seed(7)
+    table = rope_table(100, rope_frequencies(rot), magnitude=1.2)
+    pos = torch.randint(0, 100, (9,), generator=g, device="cuda", dtype=torch.int32)
+    x, up = (torch.randn((9, 3, dim), generator=g, device="cuda").to(dtype) for _ in range(2))
+    wide = torch.randn((9, 5, dim + 8), generator=g, device="cuda").to(dtype).requires_grad_()   # a view of it goes in
+    leaf = x.clone().requires_grad_()
+    for param, part in ((leaf, leaf), (wide, wide[:, 1:4, :dim])):
+        y = rope(part, table, pos, interleaved=inter, inverse=inverse)
+        assert torch.equal(y.detach(), rope(part.detach(), table, pos, interleaved=inter, inverse=inverse))
+        (grad,) = torch.autograd.grad(y, param, up)
+        d = part.detach().double().requires_grad_()
+        t = table.clone()
+        if inverse:
+            t[:, rot // 2 :] *= -1
+        (want,) = torch.autograd.grad(rope_ref_differentiable(d, t, pos, inter), d, up.double())
+        grad = grad if param is leaf else grad[:, 1:4, :dim]
+        size = float(up.abs().max()) * 1.2 * 2
+        bound = UNIT[dtype] * 1.01 * want.abs() + 3 * 2.0 ** -24 * size + (2.0 ** -25 if dtype == F16 else 0.0)
+        assert bool((grad.double() - want).abs().le(bound).all())
+    # through a sum, whose gradient has no strides; and a gradient of a gradient
+    (grad,) = torch.autograd.grad(rope(leaf, table, pos, interleaved=inter, inverse=inverse).sum(), leaf)
+    assert torch.equal(grad, rope(torch.ones_like(x), table, pos, interleaved=inter, inverse=not inverse))
+    v = up.clone().requires_grad_()
+    (grad,) = torch.autograd.grad(rope(leaf, table, pos, interleaved=inter, inverse=inverse), leaf, v, create_graph=True)
+    (again,) = torch.autograd.grad(grad, v, x)
+    assert torch.equal(again, rope(x, table, pos, interleaved=inter, inverse=inverse))
+
+
+def test_what_has_no_gradient_says_so():
+    from paper_2608_21163_b200.cache import rope, rope_frequencies, rope_table
+    c = Case([100, 50], [1, 1], qh=4, kvh=2, dim=64)
+    table, at = rope_table(128, rope_frequencies(64)), torch.tensor([99, 49], dtype=torch.int32, device="cuda")
+    k = c.q[:, :2].contiguous()
+    want, lse = c.cache.attend(c.q, c.table, c.kv_lens)
+    turned = c.cache.append(c.q, k, k, table, at, c.table, c.kv_lens)
+    q = c.q.clone().requires_grad_()
+    for call, plain in ((lambda: c.cache.append(q, k, k, table, at, c.table, c.kv_lens), turned),
+                        (lambda: c.cache.append(c.q, k.clone().requires_grad_(), k, table, at, c.table, c.kv_lens), turned),
+                        (lambda: c.cache.attend(q * 1, c.table, c.kv_lens)[0], None), (lambda: c.cache.attend(q, c.table, c.kv_lens)[1], None)):
+        y = call()
+        assert y.requires_grad and (plain is None or torch.equal(y.detach(), plain))
+        y += 1      # (an output may still be changed in place)
+        with pytest.raises(RuntimeError, match="no gradient"):
+            y.float().sum().backward()
+    with torch.no_grad():
+        out = torch.empty_like(want)
+        got, _ = c.cache.attend(q, c.table, c.kv_lens, out=out)
+        assert got is out and not got.requires_grad and rope(q, table, at, out=out) is out
+    for call in (lambda: c.cache.attend(q, c.table, c.kv_lens, out=out), lambda: c.cache.append(q, k, k, table, at, c.table, c.kv_lens, q_out=out),
+                 lambda: rope(q, table, at, out=out), lambda: rope(c.q, table.clone().requires_grad_(), at)):
+        with pytest.raises(ValueError):
+            call()
+    assert not c.cache.attend(c.q, c.table, c.kv_lens)[0].requires_grad
