@@ -286,11 +286,17 @@ int grand_cache_launches(const grand_cache* cache, uint64_t* n_out_host);
  * elements, dense along dim; out may be x.  table: table_rows x rot floats, the cosines of the rot / 2 angles of
  * position p in the first half of row p and the sines in the second (any scaling for long contexts is in it).
  * The first rot (even) entries of a head are turned pair by pair, y_a = a c - b s, y_b = b c + a s, with pairs
- * (i, i + rot / 2), or (2i, 2i + 1) if interleaved; the rest is copied.  inverse turns back: the gradient. */
+ * (i, i + rot / 2), or (2i, 2i + 1) if interleaved; the rest is copied.  inverse turns back: the gradient.
+ * A position outside the table takes the nearest row of it.  There is no handle to record that: grand_rope_checked
+ * sets bit 2 of a status word of the caller's (device memory; NULL: no record) where it finds one. */
 int grand_rope(const void* x, void* out, uint32_t dtype, uint64_t tokens, uint32_t heads, uint32_t dim,
                int64_t x_token_stride, int64_t x_head_stride, int64_t out_token_stride, int64_t out_head_stride,
                const float* table, uint64_t table_rows, uint32_t rot, const int32_t* positions,
                uint32_t interleaved, uint32_t inverse, grand_stream stream);
+int grand_rope_checked(const void* x, void* out, uint32_t dtype, uint64_t tokens, uint32_t heads, uint32_t dim,
+                       int64_t x_token_stride, int64_t x_head_stride, int64_t out_token_stride, int64_t out_head_stride,
+                       const float* table, uint64_t table_rows, uint32_t rot, const int32_t* positions,
+                       uint32_t interleaved, uint32_t inverse, uint32_t* status_dev, grand_stream stream);
 
 /* New tokens enter the cache: q (may be NULL) is turned into q_out, k is turned and written with v into the slots
  * of the new tokens, kv_lens[b] - new .. kv_lens[b] - 1, whose weights become 0.  A token whose slot is not in the

@@ -23,7 +23,7 @@ EXPORTS = [
     "grand_import_graph", "grand_reverse_graph", "grand_reverse_graph_noalloc", "grand_get_entry", "grand_set_entry", "grand_live_count",
     "grand_row_bytes", "grand_get_stats", "grand_reset_stats", "grand_set_profiling", "grand_strerror",
     "grand_last_error", "grand_cache_create", "grand_cache_destroy", "grand_cache_last_error", "grand_cache_status",
-    "grand_cache_launches", "grand_rope", "grand_cache_append", "grand_cache_attend", "grand_cache_weigh", "grand_cache_evict",
+    "grand_cache_launches", "grand_rope", "grand_rope_checked", "grand_cache_append", "grand_cache_attend", "grand_cache_weigh", "grand_cache_evict",
 ]
 
 

@@ -44,6 +44,7 @@ def _lib():
         lib.grand_cache_status.argtypes = [p, p, p]
         lib.grand_cache_launches.argtypes = [p, p]
         lib.grand_rope.argtypes = [p, p, u32, u64, u32, u32, i64, i64, i64, i64, p, u64, u32, p, u32, u32, p]
+        lib.grand_rope_checked.argtypes = lib.grand_rope.argtypes + [p]
         lib.grand_cache_append.argtypes = [p, p, p, p, p, p, p, p, p, u64, u32, p, u32, p]
         lib.grand_cache_attend.argtypes = [p, p, p, p, i64, i64, f, u32, u32, p, p, p]
         lib.grand_cache_weigh.argtypes = [p, p, p, p, i64, i64, p, f, u32, u32, f, p]
@@ -121,14 +122,14 @@ def _check_table(table, positions, tokens, device):
 
 class _Rope(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, table, positions, interleaved, inverse):
+    def forward(ctx, x, table, positions, interleaved, inverse, status):
         ctx.save_for_backward(table, positions)
         ctx.interleaved, ctx.inverse = interleaved, inverse
-        return rope(x, table, positions, interleaved, inverse)
+        return rope(x, table, positions, interleaved, inverse, status=status)
 
     @staticmethod
     def backward(ctx, grad):
-        return rope(grad, *ctx.saved_tensors, ctx.interleaved, not ctx.inverse), None, None, None, None
+        return rope(grad, *ctx.saved_tensors, ctx.interleaved, not ctx.inverse), None, None, None, None, None
 
 
 class _NoGradient(torch.autograd.Function):
@@ -151,14 +152,15 @@ def _wants_gradient(*tensors):
     return False
 
 
-def rope(x, table, positions, interleaved=False, inverse=False, out=None):
+def rope(x, table, positions, interleaved=False, inverse=False, out=None, status=None):
     """Rotary positions of x [tokens, heads, dim] (float16, bfloat16 or float32, any token and head strides): the first
     table.shape[1] entries of every head are turned by their token's angles, the others copied.  Pairs are (i, i + rot / 2),
     or (2i, 2i + 1) if interleaved.  inverse turns back, which is the gradient of the rotation; it is also what a backward pass
-    does where x requires a gradient (out is refused then, and the table is a constant).  out may be x."""
+    does where x requires a gradient (out is refused then, and the table is a constant).  out may be x.  A position outside the table takes the nearest row of it; status, an int32 CUDA
+    tensor of one entry, then gets bit 2 set (nothing clears it)."""
     if _wants_gradient(x, table):
         _need(out is None and not table.requires_grad, "rope gives a gradient to x alone, and not where out is given")
-        return _Rope.apply(x, table, positions, interleaved, inverse)
+        return _Rope.apply(x, table, positions, interleaved, inverse, status)
     _need(x.is_cuda and x.dim() == 3 and x.dtype in _DTYPE, "x must be a CUDA tensor [tokens, heads, dim] of a supported type")
     positions = _check_table(table, positions, x.shape[0], x.get_device())
     if x.stride(2) != 1:
@@ -167,10 +169,12 @@ def rope(x, table, positions, interleaved=False, inverse=False, out=None):
         out = torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
     else:
         _need(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device and out.stride(2) == 1, "out must be like x")
+    if status is not None:
+        status = _int32(status, 1, "status", x.get_device()).data_ptr()
     lib = _lib()
-    rc = lib.grand_rope(x.data_ptr(), out.data_ptr(), _DTYPE[x.dtype], x.shape[0], x.shape[1], x.shape[2], x.stride(0), x.stride(1),
-                        out.stride(0), out.stride(1), table.data_ptr(), table.shape[0], table.shape[1], positions.data_ptr(),
-                        interleaved, inverse, _stream(x.device))
+    rc = lib.grand_rope_checked(x.data_ptr(), out.data_ptr(), _DTYPE[x.dtype], x.shape[0], x.shape[1], x.shape[2], x.stride(0), x.stride(1),
+                                out.stride(0), out.stride(1), table.data_ptr(), table.shape[0], table.shape[1], positions.data_ptr(),
+                                interleaved, inverse, status, _stream(x.device))
     if rc != 0:
         raise GrandError(rc, lib.grand_strerror(rc).decode())
     return out

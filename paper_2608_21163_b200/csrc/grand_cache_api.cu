@@ -164,6 +164,13 @@ int grand_cache_launches(const grand_cache* c, uint64_t* n) {
 int grand_rope(const void* x, void* out, uint32_t dtype, uint64_t tokens, uint32_t heads, uint32_t dim, int64_t x_tok, int64_t x_head,
                int64_t o_tok, int64_t o_head, const float* table, uint64_t rows, uint32_t rot, const int32_t* positions,
                uint32_t interleaved, uint32_t inverse, grand_stream stream) {
+  return grand_rope_checked(x, out, dtype, tokens, heads, dim, x_tok, x_head, o_tok, o_head, table, rows, rot, positions, interleaved,
+                            inverse, nullptr, stream);
+}
+
+int grand_rope_checked(const void* x, void* out, uint32_t dtype, uint64_t tokens, uint32_t heads, uint32_t dim, int64_t x_tok, int64_t x_head,
+                       int64_t o_tok, int64_t o_head, const float* table, uint64_t rows, uint32_t rot, const int32_t* positions,
+                       uint32_t interleaved, uint32_t inverse, uint32_t* status, grand_stream stream) {
   if (dtype != GRAND_F32 && dtype != GRAND_F16 && dtype != GRAND_BF16) return GRAND_ERR_UNSUPPORTED;
   if (dim == 0 || dim > 256) return GRAND_ERR_UNSUPPORTED;
   if (rot % 2 || rot > dim) return GRAND_ERR_INVALID_ARG;
@@ -172,8 +179,8 @@ int grand_rope(const void* x, void* out, uint32_t dtype, uint64_t tokens, uint32
   if (int rc = check_rope(nullptr, dim, rot, table, rows, positions)) return rc;
   if (!x || !out) return GRAND_ERR_INVALID_ARG;
   const uintptr_t size = dtype == GRAND_F32 ? 4 : 2;
-  if (!aligned(x, size) || !aligned(out, size) || !aligned(table, 4) || !aligned(positions, 4)) return GRAND_ERR_INVALID_ARG;
-  RopeArgs a{x, out, x_tok, x_head, o_tok, o_head, heads, dim, tokens, table, rows, rot, positions, interleaved != 0, inverse ? -1.0f : 1.0f, nullptr};
+  if (!aligned(x, size) || !aligned(out, size) || !aligned(table, 4) || !aligned(positions, 4) || !aligned(status, 4)) return GRAND_ERR_INVALID_ARG;
+  RopeArgs a{x, out, x_tok, x_head, o_tok, o_head, heads, dim, tokens, table, rows, rot, positions, interleaved != 0, inverse ? -1.0f : 1.0f, status};
   return done(nullptr, launch_rope(a, dtype, static_cast<cudaStream_t>(stream)), "rope");
 }
 

@@ -302,3 +302,22 @@ def test_what_has_no_gradient_says_so():
         with pytest.raises(ValueError):
             call()
     assert not c.cache.attend(c.q, c.table, c.kv_lens)[0].requires_grad
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+def test_rope_records_positions_outside_the_table(dtype):
+    from paper_2608_21163_b200.cache import rope, rope_frequencies, rope_table
+    table, x = rope_table(50, rope_frequencies(32)), torch.randn((5, 3, 40), device="cuda").to(dtype)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    good = torch.tensor([0, 49, 7, 49, 0], dtype=torch.int32, device="cuda")
+    want = rope(x, table, good, status=status)
+    assert status.tolist() == [0]
+    bad = torch.tensor([0, 50, 7, (1 << 31) - 1, -1], dtype=torch.int32, device="cuda")
+    assert torch.equal(rope(x, table, bad, status=status), want) and status.tolist() == [2]
+    assert torch.equal(rope(x, table, bad), want)
+    status.zero_()
+    rope(x.clone().requires_grad_(), table, bad, status=status)
+    assert status.tolist() == [2]
+    for wrong in (status.cpu(), status.float(), torch.zeros(2, dtype=torch.int32, device="cuda")):
+        with pytest.raises(ValueError):
+            rope(x, table, good, status=wrong)
