@@ -180,6 +180,16 @@ def rope(x, table, positions, interleaved=False, inverse=False, out=None, status
     return out
 
 
+# Handles of collected objects.  To destroy one waits for the whole device, which a collection must not do at a time of its own
+# choosing: it would stall every stream, and end a graph capture with an error.
+_collected = []
+
+
+def _destroy_collected(lib):
+    while _collected:
+        lib.grand_cache_destroy(_collected.pop())
+
+
 class TokenCache:
     """Operators on one pool of pages, with their workspace.
 
@@ -194,6 +204,9 @@ class TokenCache:
 
     The methods have no gradient (`rope` has): a backward pass through what append or attend returned raises, and out, lse and q_out are
     refused where one of the inputs requires a gradient.  What lies in the pool and its weights is never part of one.
+
+    An object's workspace is four partial results an SM (39 MB on 148), whatever its sizes.  close() frees it; that of an object that
+    was collected without is freed with the next object that is made or closed.
     """
 
     def __init__(self, k_pages, v_pages, weights=None, q_heads=None, max_batch=256, max_tokens=8192):
@@ -207,6 +220,7 @@ class TokenCache:
             _need(weights.dtype == torch.float32 and weights.device == k_pages.device and weights.is_contiguous()
                   and tuple(weights.shape) == (pages, groups, size) and groups in (1, kv_heads), "weights must be dense float32 [pages, 1 or kv heads, page size]")
         self.lib = _lib()
+        _destroy_collected(self.lib)
         self.k_pages, self.v_pages, self.weights = k_pages, v_pages, weights
         self.q_heads, self.kv_heads, self.head_dim, self.page_size, self.groups = q_heads or kv_heads, kv_heads, dim, size, groups
         self.dtype, self.device, self.index = k_pages.dtype, k_pages.device, k_pages.get_device()
@@ -227,15 +241,16 @@ class TokenCache:
         self._strides = (C.c_int64 * 6)()
 
     def close(self):
+        """Frees the workspace, and those of collected objects, once the device is idle."""
         if getattr(self, "h", None):
             self.lib.grand_cache_destroy(self.h)
             self.h = None
+            _destroy_collected(self.lib)
 
     def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
+        if getattr(self, "h", None):
+            _collected.append(self.h)
+            self.h = None
 
     def _check(self, rc):
         if rc != 0:

@@ -64,3 +64,31 @@ def test_rope_table_is_exact_far_out():
             assert abs(float(t[p, i]) - 1.25 * math.cos(angle)) < 1e-7 and abs(float(t[p, 4 + i]) - 1.25 * math.sin(angle)) < 1e-7
     with pytest.raises(ValueError):
         cache.rope_frequencies(7)
+
+
+def test_a_collected_cache_waits_for_nobody():
+    """Its handle is destroyed with the next object that is made or closed, not by the collection."""
+    class Lib:
+        gone = []
+
+        def grand_cache_destroy(self, h):
+            self.gone.append(h)
+
+    def made(h):
+        c = cache.TokenCache.__new__(cache.TokenCache)
+        c.lib, c.h = Lib(), h
+        return c
+
+    before = list(cache._collected)
+    cache._collected.clear()
+    a, b, c = made(1), made(2), made(3)
+    del a, b
+    assert Lib.gone == [] and sorted(cache._collected) == [1, 2]
+    c.close()
+    assert sorted(Lib.gone) == [1, 2, 3] and not cache._collected
+    c.close()
+    del c
+    assert len(Lib.gone) == 3 and not cache._collected
+    del made
+    cache.TokenCache.__new__(cache.TokenCache).__del__()   # an object that was never made
+    cache._collected.extend(before)

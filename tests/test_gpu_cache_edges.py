@@ -321,3 +321,22 @@ def test_rope_records_positions_outside_the_table(dtype):
     for wrong in (status.cpu(), status.float(), torch.zeros(2, dtype=torch.int32, device="cuda")):
         with pytest.raises(ValueError):
             rope(x, table, good, status=wrong)
+
+
+def test_collection_during_a_capture():
+    import gc
+    from paper_2608_21163_b200.cache import TokenCache, _collected
+    c = Case([500, 70], [1, 1], qh=8, kvh=2, dim=64)
+    want, lse = c.cache.attend(c.q, c.table, c.kv_lens)
+    other = TokenCache(c.k, c.v, q_heads=8)
+    other.attend(c.q, c.table, c.kv_lens)
+    out, l2, graph = torch.empty_like(want), torch.empty_like(lse), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.cache.attend(c.q, c.table, c.kv_lens, out=out, lse=l2)
+        del other
+        gc.collect()
+        assert len(_collected) >= 1
+    graph.replay()
+    assert torch.equal(out, want) and torch.equal(l2, lse)
+    TokenCache(c.k, c.v, q_heads=8).close()
+    assert not _collected
