@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kWarps * 32, 8 / kWarps) attend_stream_kernel(
             for (int n = 0; n < NT; ++n) o[mt][n][2 * i] *= f, o[mt][n][2 * i + 1] *= f;
           }
         }
-        const float ref[2] = {m[mt][0] == kNegInf ? 0.0f : m[mt][0], m[mt][1] == kNegInf ? 0.0f : m[mt][1]};
+        const float ref[2] = {m[mt][0] == kNegInf ? 0.0f : m[mt][0] - kLift<BF16>, m[mt][1] == kNegInf ? 0.0f : m[mt][1] - kLift<BF16>};
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kWarps * 32, 8 / kWarps) attend_stream_kernel(
     };
     auto emit_lse = [&](int r, float top, float sum) {
       const int row = r_base + r, tok = (int)div_fast(row, a.group), g = row - tok * (int)a.group.d;
-      if (a.lse) a.lse[(int64_t)(it.row + tok) * kvh * a.group.d + it.h * (int)a.group.d + g] = (top + log2f(sum)) * kLn2;
+      if (a.lse) a.lse[(int64_t)(it.row + tok) * kvh * a.group.d + it.h * (int)a.group.d + g] = (top - kLift<BF16> + log2f(sum)) * kLn2;
     };
     float* slot = a.partial + ((uint64_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * a.slot_floats;
     for (int x = tid; x < n_rows * (DP / 2); x += blockDim.x) {

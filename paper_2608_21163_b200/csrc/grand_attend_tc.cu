@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               }
             }
           }
-          const float ref = m == kNegInf ? 0.0f : m;
+          const float ref = m == kNegInf ? 0.0f : m - kLift<BF16>;
           const float2 sub = make_float2(-ref, -ref), mul = make_float2(scale, scale);
           auto exponentials = [&](auto is_fast) {
 #pragma unroll
@@ -408,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(o[i]);
             emit(c * 16, v, f);
           }
-          if (live && a.lse && side == 0) a.lse[out_row] = (m + log2f(l)) * kLn2;
+          if (live && a.lse && side == 0) a.lse[out_row] = (m - kLift<BF16> + log2f(l)) * kLn2;
         } else {
           // a part: entry-major, so that a warp's rows lie side by side
           constexpr uint64_t kPart = (uint64_t)(DP + 2) * 128;   // of one row tile
@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               const float f = inverse(sum);
               emit(k * 32, v[0], f);
               emit(k * 32 + 16, v[1], f);
-              if (live && a.lse && side == 0 && k == 0) a.lse[out_row] = (top + log2f(sum)) * kLn2;
+              if (live && a.lse && side == 0 && k == 0) a.lse[out_row] = (top - kLift<BF16> + log2f(sum)) * kLn2;
             }
           }
         }

@@ -8,6 +8,12 @@ namespace grand {
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kNegInf = -__builtin_huge_valf();
 
+// Unnormalised probabilities are 2^(s - m + kLift): a float16 has no numbers below 2^-24, so without the lift all keys whose probability is
+// below 2^-25 of a row's largest would vanish from the output and stay in the sum.  m is at most 8 behind the maximum, so the
+// largest number is 2^15, the last power of two that a float16 holds.  A bfloat16 has the range of 32 bits.
+template <bool BF16>
+constexpr float kLift = BF16 ? 0.0f : 7.0f;
+
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -340,3 +340,28 @@ def test_collection_during_a_capture():
     assert torch.equal(out, want) and torch.equal(l2, lse)
     TokenCache(c.k, c.v, q_heads=8).close()
     assert not _collected
+
+
+# ---- numerics
+
+@pytest.mark.parametrize("new", [1, 40])     # the streaming kernel, and the one on the tensor cores
+def test_many_small_probabilities_count_in_float16(new):
+    """64 keys that draw almost all of the weight, and nearly 3,000 that have 2^-25.4 of the weight of one: not one of them is a float16
+    number beside 1, and together they are the output."""
+    n, seqs, big, value = 3000, 300, 64, 1000.0
+    c = Case([n] * seqs, [new] * seqs, qh=4, kvh=1, dim=64, page=60, dtype=F16)
+    c.q.zero_(); c.k.zero_(); c.v.fill_(value)
+    c.q[..., 0] = 1.0
+    c.k[..., 0] = -17.6
+    first = c.table[:, :2].long()
+    c.k[first[:, 0]], c.v[first[:, 0]] = 0.0, 0.0
+    c.k[first[:, 1], : big - 60], c.v[first[:, 1], : big - 60] = 0.0, 0.0
+    out, lse = c.cache.attend(c.q, c.table, c.kv_lens, cu_new=c.cu, scale=1.0)
+    small = (torch.arange(n - new + 1, n + 1, device="cuda", dtype=torch.float64) - big) * math.exp(float(torch.tensor(-17.6, dtype=F16)))
+    want, want_lse = (small / (big + small) * value).repeat(seqs)[:, None, None], (big + small).log().repeat(seqs)[:, None]
+    # a probability is rounded to a multiple of 2^-24 where the largest is 2^7 or more, and the sum is at least 64 of those; the
+    # sums run in 32 bits
+    bound = n * 2.0 ** -32 * value / big + (1.05 * UNIT[F16] + n * 2.0 ** -23) * want
+    assert bool((out.double() - want).abs().le(bound).all()), float(((out.double() - want).abs() / bound).max())
+    assert bool((lse.double() - want_lse).abs().le(n * 2.0 ** -24 + 2.0 ** -20).all())
+    assert c.cache.status() == 0
