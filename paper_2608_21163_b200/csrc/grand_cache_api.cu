@@ -209,7 +209,8 @@ int grand_cache_attend(grand_cache* c, const grand_pool* p, const grand_seqs* s,
   AttendArgs a{};
   if (int rc = views(c, p, s, false, true, &a.pool, &a.seq)) return rc;
   if (window && !causal) return fail(c, GRAND_ERR_INVALID_ARG, "a window needs causal attention");
-  if (!(std::fabs(scale) <= 3.0e38f)) return fail(c, GRAND_ERR_INVALID_ARG, "scale is not finite");
+  // (times log2(e) it has to be a finite float)
+  if (!(std::fabs(scale) <= 2.0e38f)) return fail(c, GRAND_ERR_INVALID_ARG, "scale must be at most 2e38");
   if (s->tokens == 0 || s->batch == 0) return GRAND_OK;
   if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || q_tok % 8 || q_head % 8)
     return fail(c, GRAND_ERR_INVALID_ARG, "q and out must be 16-byte aligned, q's strides multiples of 8");
@@ -234,7 +235,7 @@ int grand_cache_weigh(grand_cache* c, const grand_pool* p, const grand_seqs* s, 
   WeighArgs a{};
   if (int rc = views(c, p, s, true, true, &a.pool, &a.seq)) return rc;
   if (window && !causal) return fail(c, GRAND_ERR_INVALID_ARG, "a window needs causal attention");
-  if (!(std::fabs(scale) <= 3.0e38f) || !(std::fabs(decay) <= 3.0e38f)) return fail(c, GRAND_ERR_INVALID_ARG, "scale or decay is not finite");
+  if (!(std::fabs(scale) <= 2.0e38f) || !(std::fabs(decay) <= 3.0e38f)) return fail(c, GRAND_ERR_INVALID_ARG, "scale must be at most 2e38, decay finite");
   if (s->batch == 0) return GRAND_OK;
   if (s->tokens && (!q || !lse || !aligned(q, 16) || q_tok % 8 || q_head % 8))
     return fail(c, GRAND_ERR_INVALID_ARG, "q must be 16-byte aligned with strides that are multiples of 8, lse given");

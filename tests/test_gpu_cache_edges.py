@@ -5,6 +5,8 @@ import math
 import pytest
 import torch
 
+from paper_2608_21163_b200.binding import GrandError
+
 from .test_gpu_cache import BF16, F16, UNIT, Case, rope_ref_differentiable
 
 pytestmark = pytest.mark.gpu
@@ -365,3 +367,16 @@ def test_many_small_probabilities_count_in_float16(new):
     assert bool((out.double() - want).abs().le(bound).all()), float(((out.double() - want).abs() / bound).max())
     assert bool((lse.double() - want_lse).abs().le(n * 2.0 ** -24 + 2.0 ** -20).all())
     assert c.cache.status() == 0
+
+
+def test_a_scale_that_overflows_is_refused():
+    """Times log2(e) a scale above 2.3e38 is infinite, and infinity times a score of 0 no number."""
+    c = Case([100, 50], [1, 1], qh=4, kvh=2, dim=64)
+    c.q.zero_()
+    want, lse = c.cache.attend(c.q, c.table, c.kv_lens)
+    got, _ = c.cache.attend(c.q, c.table, c.kv_lens, scale=1.9e38)
+    assert torch.equal(got, want)
+    for scale in (2.5e38, -2.5e38, math.inf):
+        for call in (lambda: c.cache.attend(c.q, c.table, c.kv_lens, scale=scale), lambda: c.cache.weigh(c.q, lse, c.table, c.kv_lens, scale=scale)):
+            with pytest.raises(GrandError, match="2e38"):
+                call()
