@@ -71,8 +71,7 @@ struct RowLayout {
   __device__ __forceinline__ static uint32_t at(int row, int chunk) { return row * kBytes + ((chunk ^ (row & 7)) << 4); }
 };
 
-// Fragments of up to 16 query rows, straight from global memory: row r is query head r % group of token r / group.
-// As the left operand (16 rows x 16 entries per step), for KS steps of 16 entries; rows and entries beyond the end are zero.
+// Entries i and i + 1 of a row, zeros behind its end.
 __device__ __forceinline__ uint32_t load_pair(const uint16_t* p, int i, int dim) {
   return i < dim ? __ldg(reinterpret_cast<const uint32_t*>(p + i)) : 0u;  // dim is even, i is even
 }

@@ -152,11 +152,9 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-__device__ __forceinline__ void group_sync(int t) {  // the 128 threads of warpgroup t < 4
+__device__ __forceinline__ void group_sync(int t) {  // the 128 threads of warpgroup t, 0 or 1
   if (t == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
-  else if (t == 1) asm volatile("bar.sync 2, 128;" ::: "memory");
-  else if (t == 2) asm volatile("bar.sync 3, 128;" ::: "memory");
-  else asm volatile("bar.sync 4, 128;" ::: "memory");
+  else asm volatile("bar.sync 2, 128;" ::: "memory");
 }
 
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {  // a NaN if one of them is

@@ -3,14 +3,16 @@
 //
 // S^T = K Q^T, 128 keys on the long side (a key's scores lie in one lane of tensor memory, so one thread sums them) and up
 // to 128 query rows on the other.  A pair costs 2 dim flops and one exponential: for a tile of 128 x 128 at dim 128 the
-// products take 256 cycles of the tensor cores and the exponentials 1024 at 16 a cycle, so the exponentials bound it.
+// products take 512 cycles of the tensor cores and the exponentials 1,024 at 16 a cycle, so the exponentials bound it.  Measured
+// (four chunks of 1,024 tokens on up to 8,000) their unit is busy for two thirds of the time: every thread also reads -lse of every
+// row from shared memory, 16 bytes for four exponentials, through the same queue.
 //
 // One block per SM: a warp that brings keys (once per item and kv head) and query rows (a ring) in, one that brings what
 // the exponents need of each row, two lanes that issue the products into four score tiles in tensor memory, and four
-// warpgroups that take the score tiles in turn.  (Measured on four chunks of 1,024 tokens on 8,000: two warpgroups that
-// fetch the rows' data themselves 302 us of device time, four 307, with a warp of its own for that data 283, with the
-// producers' loops shortened and two issuing lanes 265.)  An item is a tile of 128 keys of one sequence and weight row; its
-// tiles are the row tiles that see it, of each of its kv heads.  All tiles are numbered through and every block takes an
+// warpgroups that take the score tiles in turn.  (On the same chunks: two warpgroups that fetch the rows' data themselves 302 us of
+// device time, four 307, with a warp of its own for that data 283, with the producers' loops shortened and two issuing lanes
+// 265, with 256 keys to a tile of rows instead of 128 220.)  An item is a tile of 256 keys, two halves of 128, of one sequence and
+// weight row; its tiles are the row tiles that see it, of each of its kv heads.  All tiles are numbered through and every block takes an
 // equal run of them; parts of an item are joined in their order by the block that arrives last, so equal calls give equal
 // bits.
 #include "grand_attend_items.cuh"
