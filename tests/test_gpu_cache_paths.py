@@ -26,6 +26,16 @@ def test_unequal_sequences(lens, news, dim):
     c.check_weigh(window=300, decay=0.5)
 
 
+@pytest.mark.parametrize("lens,news", [([40000], [1]), ([9000, 100], [3, 8]), ([6000, 900], [700, 900]), ([20000], [40])])
+def test_equal_calls_give_equal_bits(lens, news):
+    """Parts of a sequence are joined in their order, whichever block arrives last."""
+    c = Case(lens, news, qh=8, kvh=2, dim=64, page=16)
+    want, lse = c.cache.attend(c.q, c.table, c.kv_lens, cu_new=c.cu)
+    for _ in range(20):
+        got, again = c.cache.attend(c.q, c.table, c.kv_lens, cu_new=c.cu)
+        assert torch.equal(got, want) and torch.equal(again, lse)
+
+
 # ---- layouts
 
 @pytest.mark.parametrize("page", [1, 2, 4, 6])
