@@ -311,7 +311,7 @@ int grand_cache_append(grand_cache* cache, const grand_pool* pool, const grand_s
 /* Attention of the new tokens over the cache: new token i of a sequence with n cached and m new tokens attends
  * the tokens j < n with j <= n - m + i if causal, and j > n - m + i - window if window > 0 (causal only).
  * out = softmax(scale q.k) v, lse = log(sum(exp(scale q.k))) (natural); a row that attends nothing has out 0 and
- * lse -inf.  q: tokens x q_heads x head_dim (token and head stride), out and lse dense, lse may be NULL.
+ * lse -inf, and a row that belongs to no sequence is left as it is.  q: tokens x q_heads x head_dim (token and head stride), out and lse dense, lse may be NULL.
  * Scores, the softmax's maximum and sum, and the output's sum are fp32.  The unnormalised probabilities meet the
  * values in the cache's type: as the sum of two numbers of it with up to 32 rows (query heads of a kv head x new
  * tokens) per sequence on average, rounded to one beyond that.  A key that a row does not see may hold anything; the
