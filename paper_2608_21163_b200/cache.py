@@ -155,9 +155,9 @@ def _wants_gradient(*tensors):
 def rope(x, table, positions, interleaved=False, inverse=False, out=None, status=None):
     """Rotary positions of x [tokens, heads, dim] (float16, bfloat16 or float32, any token and head strides): the first
     table.shape[1] entries of every head are turned by their token's angles, the others copied.  Pairs are (i, i + rot / 2),
-    or (2i, 2i + 1) if interleaved.  inverse turns back, which is the gradient of the rotation; it is also what a backward pass
-    does where x requires a gradient (out is refused then, and the table is a constant).  out may be x.  A position outside the table takes the nearest row of it; status, an int32 CUDA
-    tensor of one entry, then gets bit 2 set (nothing clears it)."""
+    or (2i, 2i + 1) if interleaved.  inverse turns back, which is the gradient of the rotation and what a backward pass does where
+    x requires one (out is refused then, and the table is a constant).  out may be x.  A position outside the table takes the
+    nearest row of it; status, an int32 CUDA tensor of one entry, then gets bit 2 set (nothing clears it)."""
     if _wants_gradient(x, table):
         _need(out is None and not table.requires_grad, "rope gives a gradient to x alone, and not where out is given")
         return _Rope.apply(x, table, positions, interleaved, inverse, status)
@@ -350,7 +350,8 @@ class TokenCache:
     def evict(self, page_table, kv_lens, keep, sinks=0, recent=0, into=None):
         """Brings every sequence down to `keep` tokens: its first `sinks`, its last `recent` and the heaviest of the others (ties:
         the lowest index), moved together in their order, in place or into the pages of the table `into` (other pages than
-        the sequences').  Tokens without a page are not kept.  Returns the kept tokens' indices [batch, groups, keep], -1 behind the last, and the new lengths."""
+        the sequences').  Tokens without a page are not kept.  Returns the kept tokens' indices [batch, groups, keep], -1 behind
+        the last, and the new lengths."""
         keep, sinks, recent = _count(keep, "keep"), _count(sinks, "sinks"), _count(recent, "recent")
         hold = self._sequences(page_table, kv_lens, None, page_table.shape[0])
         batch = page_table.shape[0]
