@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     // A token without a page takes no part.  Its key, loaded as zeros, becomes NaN, and so do its scores: the softmax of a tile
     // without such tokens has nothing to ask, and one that meets a NaN looks for them.
     auto mark_gaps = [&](int k_stage, int j) {
-      if (!gaps) return;
+      if (!__any_sync(0xFFFFFFFFu, gaps)) return;   // (the warp decides as one: the flag may be raised for a later tile between two lanes' reads)
       const int32_t* table = a.seq.table + (int64_t)it.b * a.seq.table_stride;
       for (int r = lane; r < kTile; r += 32) {
         const int key = it.lo + j * kTile + r;
